@@ -148,7 +148,8 @@ typedef struct {
     int32_t *out_seg;            /* device [out_capacity_rows] or NULL: segment of each
                                     output row (-1 in reserve rows)                     */
     int32_t *status;             /* device int32 or NULL                                */
-    void *workspace;             /* device, sonic_compact_workspace_size() bytes        */
+    void *workspace;             /* device, sonic_compact_workspace_size() bytes, 8-byte
+                                    aligned                                             */
     size_t workspace_bytes;
     int32_t total_rows;          /* rows per layer of K, V, role, seg_id (> 0); a
                                     sequence outside them is refused                    */
@@ -435,7 +436,8 @@ typedef struct {
     uint8_t *out_role;           /* device [cache rows] or NULL                         */
     int32_t *out_seg;            /* device [cache rows] or NULL                         */
     int32_t *status;             /* device int32 or NULL                                */
-    void *workspace;             /* device, sonic_kv4_compact_workspace_size() bytes    */
+    void *workspace;             /* device, sonic_kv4_compact_workspace_size() bytes,
+                                    8-byte aligned                                      */
     size_t workspace_bytes;
 } sonic_kv4_compact_args;
 

@@ -566,6 +566,22 @@ kv_gather_kernel(const uint8_t *K, const uint8_t *V,
 
 }  // namespace
 
+// One launch plans all rows where every block can count the kept rows ahead of its own.
+static bool one_launch(const sonic_compact_args *a) {
+    return a->total_rows <= kPlanRows && (int64_t)a->total_rows * a->batch <= kPlanWork;
+}
+
+// The arrays lie at multiples of 256 bytes from the workspace's start: 64-bit sums in the scan of
+// three launches, in the other the source rows where the caller takes none.
+sonic_status_t check_scan_workspace(const sonic_compact_args *a) {
+    const size_t need = sonic_compact_workspace_size(a);
+    if (need > 0 && (a->workspace == nullptr || a->workspace_bytes < need)) return SONIC_ERR_WORKSPACE;
+    const size_t unit = !one_launch(a)             ? sizeof(long long)
+                        : a->src_idx == nullptr ? sizeof(int32_t)
+                                                : 1;
+    return reinterpret_cast<uintptr_t>(a->workspace) % unit == 0 ? SONIC_OK : SONIC_ERR_INVALID_ARGUMENT;
+}
+
 // The retention scan of a call whose arguments were checked: offsets and, in *src_idx_out, the
 // source row of every output row (the caller's array or the workspace's).
 cudaError_t launch_keep_scan(const int32_t *seg_id, const uint8_t *role, int32_t *offsets,
@@ -579,7 +595,7 @@ cudaError_t launch_keep_scan(const int32_t *seg_id, const uint8_t *role, int32_t
     int32_t *src_idx = *src_idx_out = a->src_idx != nullptr ? a->src_idx : reinterpret_cast<int32_t *>(ws);
 
     cudaError_t e = cudaSuccess;
-    if (a->total_rows <= kPlanRows && (int64_t)a->total_rows * a->batch <= kPlanWork) {
+    if (one_launch(a)) {
         // pieces per sequence by the mean length, and helpers for longer ones where there can be
         // such: enough for one array of rows, and up to a block per SM where sequences share rows
         // (near 65,535 sequences, the grid's limit, there is no room for them: fewer pieces)
@@ -652,9 +668,8 @@ extern "C" sonic_status_t sonic_compact_kv(const void *K, const void *V, const i
         return SONIC_ERR_INVALID_ARGUMENT;
     if (a->n_layers > 32767 || a->batch > 65535) return SONIC_ERR_UNSUPPORTED;
     if (a->total_rows <= 0) return SONIC_ERR_INVALID_ARGUMENT;
-    const size_t need = sonic_compact_workspace_size(a);
-    if (need > 0 && (a->workspace == nullptr || a->workspace_bytes < need))
-        return SONIC_ERR_WORKSPACE;
+    const sonic_status_t st = check_scan_workspace(a);
+    if (st != SONIC_OK) return st;
 
     int32_t *src_idx = nullptr;
     cudaError_t e = launch_keep_scan(seg_id, role, offsets, a, &src_idx, stream);

@@ -304,9 +304,8 @@ extern "C" sonic_status_t sonic_kv4_compact(const uint16_t *K, const uint16_t *V
     if (st != SONIC_OK) return st;
     if (a->batch > 65535) return SONIC_ERR_UNSUPPORTED;
     const sonic_compact_args s = scan_args(c, a);
-    const size_t need = sonic_compact_workspace_size(&s);
-    if (need > 0 && (a->workspace == nullptr || a->workspace_bytes < need))
-        return SONIC_ERR_WORKSPACE;
+    st = check_scan_workspace(&s);
+    if (st != SONIC_OK) return st;
     int32_t *src_idx = nullptr;
     if (launch_keep_scan(seg_id, role, offsets, &s, &src_idx, stream) != cudaSuccess)
         return SONIC_ERR_CUDA;

@@ -25,7 +25,9 @@ bool make_tmap_bf16_5d(CUtensorMap *map, const void *base, const uint64_t dims[5
 // Number of SMs of the current device (cached per device).
 int device_sm_count();
 
-// The retention scan of sonic_compact_kv, for its other forms (compact.cu).
+// The retention scan of sonic_compact_kv, for its other forms (compact.cu): its workspace's size and
+// place, and its launches.
+sonic_status_t check_scan_workspace(const sonic_compact_args *a);
 cudaError_t launch_keep_scan(const int32_t *seg_id, const uint8_t *role, int32_t *offsets,
                              const sonic_compact_args *a, int32_t **src_idx_out,
                              cudaStream_t stream);

@@ -187,3 +187,20 @@ def test_routed_linear_refuses_a_misaligned_workspace():
     a.parts[0].base, a.parts[0].row_stride, a.parts[0].cols, a.parts[0].rows = 16, 64, 64, 10
     a.workspace, a.workspace_bytes = 24, 1 << 20
     assert lib.sonic_routed_linear(16, 16, 16, 16, ctypes.byref(a), None) == 1
+
+
+def test_compaction_refuses_a_misaligned_workspace():
+    """Source rows (32 bits) and, in the scan of three launches, sums (64 bits) are written there."""
+    lib = sonic.load()
+    for rows, misaligned in ((10, (17, 18, 19, 21)), (1 << 20, (17, 18, 20, 28))):
+        a = sonic.sonic_compact_args()
+        a.batch, a.n_layers, a.row_bytes, a.total_rows = 2, 1, 32, rows
+        a.k_start = a.k_len = 16
+        a.workspace_bytes = 1 << 20
+        four = sonic.sonic_kv4_cache(16, 16, 16, 16, 8, 4096, 512)
+        f = sonic.sonic_kv4_compact_args(2, 1, 2, 128, 16, 16, None, rows, 0)
+        f.workspace_bytes = 1 << 20
+        for at in misaligned:
+            a.workspace = f.workspace = at
+            assert lib.sonic_compact_kv(16, 16, None, 16, 16, 16, 16, ctypes.byref(a), None) == 1
+            assert lib.sonic_kv4_compact(16, 16, None, 16, ctypes.byref(four), 16, ctypes.byref(f), None) == 1
