@@ -596,9 +596,10 @@ typedef struct {
  * choice of its own, of the same number of rows.  Writes
  *   offsets[b] = sum_{b' < b} (n_b' + reserve[b'])  (device [B + 1])
  * and moves the kept rows of every part to rows offsets[b] .. offsets[b] +
- * n_b - 1 of its destination, which must not overlap the sources (nor out_mass
- * and out_role theirs).  The parts' rows in reserve, and all rows behind the
- * last sequence, are not written.  If offsets[B] > out_rows the call sets
+ * n_b - 1 of its destination, which must not overlap the sources.  The parts'
+ * rows in reserve, and all rows behind the last sequence, are not written.
+ * offsets, out_len, src_idx, out_mass and out_role over any of lens, kv_start,
+ * budget, reserve, mass and role, and a part with dst = src, are refused.  If offsets[B] > out_rows the call sets
  * SONIC_ERR_CAPACITY and writes only rows below it.  A sequence whose rows
  * fall outside [0, total_kv_rows) or that is longer than max_len keeps none and sets
  * SONIC_ERR_INVALID_ARGUMENT.  total_kv_rows above 2^31 - 4097 is unsupported.

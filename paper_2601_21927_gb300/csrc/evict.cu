@@ -445,6 +445,27 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const Params p
         move_part<uint32_t>(p, q);
 }
 
+// Whether an output lies over an input.  A block writes offsets, out_len and the rows that it chose while
+// others still read the lengths, starts, budgets and masses.
+bool outputs_over_inputs(const float *mass, const int32_t *lens, const int32_t *offsets, const sonic_evict_args *a) {
+    const size_t word = sizeof(int32_t), per_seq = (size_t)a->batch * word;
+    const size_t maps = (size_t)a->mass_layers * a->mass_heads;
+    const size_t in_rows = (size_t)a->total_kv_rows, out_rows = maps * a->out_rows;
+    const struct {
+        const void *at;
+        size_t bytes;
+    } in[] = {{lens, per_seq}, {a->kv_start, per_seq}, {a->budget, per_seq}, {a->reserve, per_seq},
+              {mass, maps * in_rows * word}, {a->role, in_rows}},
+      out[] = {{offsets, per_seq + word}, {a->out_len, per_seq}, {a->src_idx, out_rows * word},
+               {a->out_mass, out_rows * word}, {a->out_role, out_rows}};
+    for (const auto &o : out)
+        for (const auto &i : in)
+            if (overlap(o.at, o.bytes, i.at, i.bytes)) return true;
+    for (int i = 0; i < a->n_parts; ++i)  // (a part moved onto itself; regions may interleave by their strides)
+        if (a->parts[i].src == a->parts[i].dst && a->parts[i].src != nullptr) return true;
+    return false;
+}
+
 size_t kept_bytes(const sonic_evict_args *a) {
     return round_up((size_t)a->batch * sizeof(int32_t), 256);
 }
@@ -513,7 +534,7 @@ extern "C" sonic_status_t sonic_evict_kv(const float *mass, const int32_t *lens,
     if (blocks > 0x7fffffffLL) return SONIC_ERR_UNSUPPORTED;
     const size_t need = sonic_evict_workspace_size(a);
     if (a->workspace == nullptr || a->workspace_bytes < need) return SONIC_ERR_WORKSPACE;
-    if (!aligned16(a->workspace)) return SONIC_ERR_INVALID_ARGUMENT;
+    if (!aligned16(a->workspace) || outputs_over_inputs(mass, lens, offsets, a)) return SONIC_ERR_INVALID_ARGUMENT;
     char *ws = static_cast<char *>(a->workspace);
     p.mass = mass;
     p.lens = lens;

@@ -60,6 +60,12 @@ cudaError_t launch_pdl(void (*kern)(Params...), dim3 grid, unsigned threads, siz
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Whether [a, a + na) and [b, b + nb) share a byte (never where one is NULL).
+inline bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x != 0 && y != 0 && na != 0 && nb != 0 && x < y + nb && y < x + na;
+}
+
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace sonic

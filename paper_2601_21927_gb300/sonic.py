@@ -599,7 +599,7 @@ def sonic_evict_kv(mass: torch.Tensor, parts, lens: torch.Tensor, offsets: torch
     an extent of 1 makes one choice for all layers or heads) within budget[b].  parts: up to four
     (src, dst) pairs of cache arrays, bf16 [n_layers, rows, Hkv, D] or four-bit codes or scales
     (uint8, [n_layers, Hkv, rows, ..]).  src_idx, out_mass, out_role: [.., .., out rows] like mass.
-    Returns the workspace."""
+    No output may lie over an input (out_len is not lens).  Returns the workspace."""
     where, dev = "sonic_evict_kv", _device()
     lib = load()
     ml, mh, rows = _dims(where, "mass", mass, 3)

@@ -203,3 +203,27 @@ def test_plain_evict():
     assert plain.evict_rows([nan, float("-inf"), 0], [False] * 3, 2) == [0, 2]
     assert plain.evict_rows([1, 2, 3], [True, True, False], 1) == [0, 1]
     assert plain.evict_rows([], [], 4) == []
+
+
+def test_evict_refuses_outputs_over_inputs():
+    """Blocks write offsets, lengths and choices while others still read the lengths, starts, budgets and
+    masses: an output in an input's place (whole, or by one word) is refused."""
+    lib = sonic.load()
+    # (name, bytes): 5 sequences, 2 x 2 choices, 40 rows in and 24 out
+    ins = dict(lens=20, kv_start=20, budget=20, reserve=20, mass=640, role=40)
+    outs = dict(offsets=24, out_len=20, src_idx=384, out_mass=384, out_role=96)
+    place = {n: 4096 * (i + 1) for i, n in enumerate((*ins, *outs))}
+
+    def call(**at):
+        at = {**place, **at}
+        a = sonic.sonic_evict_args(5, 2, 2, 2, 2, at["kv_start"], 20, 40, at["budget"], at["reserve"], at["role"], 1, 0,
+                                   24, at["out_len"], at["src_idx"], at["out_mass"], at["out_role"])
+        a.workspace, a.workspace_bytes, a.n_parts = 1 << 20, 1 << 16, 1
+        a.parts[0] = sonic.sonic_evict_part(at.get("src", 1 << 22), 1 << 23, 256, 20480, 256, 512, 12288, 256, 512)
+        return lib.sonic_evict_kv(at["mass"], at["lens"], at["offsets"], by(a), None)
+
+    for i, n_in in ins.items():
+        for o, n_out in outs.items():
+            for at in (place[i], place[i] + (n_in - 4 if o != "out_role" else n_in - 1), place[i] - n_out + 4):
+                assert call(**{o: at}) == 1, (i, o)
+    assert call(src=1 << 23) == 1
