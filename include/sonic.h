@@ -164,9 +164,9 @@ typedef struct {
  * and for every layer l and kept row j of sequence b copies the row_bytes of
  * K (resp. V) row k_start[b] + (j-th kept position) of layer l to row
  * offsets[b] + j of layer l of out_K (resp. out_V), bit for bit.  Reserve
- * rows are not written.  seg_id may be NULL; when given it is checked
- * (non-decreasing within a sequence, no body row in segment 0) and a
- * violation sets SONIC_ERR_LAYOUT.  If offsets[B] > out_capacity_rows the
+ * rows are not written, and no output may overlap an input.  seg_id may be
+ * NULL; when given it is checked (non-decreasing within a sequence, no body row
+ * in segment 0) and a violation sets SONIC_ERR_LAYOUT.  If offsets[B] > out_capacity_rows the
  * call sets SONIC_ERR_CAPACITY and copies only rows below the capacity.
  * K/V/out pointers must be 16-byte aligned.  B > 65535 or n_layers > 32767
  * returns SONIC_ERR_UNSUPPORTED.  A sequence whose rows fall outside
@@ -446,6 +446,8 @@ typedef struct {
  * optional outputs, checks and conditions in *status (cache->rows is the
  * capacity), each kept row of K and V (bf16) packed where it would have been
  * copied.  Reserve rows, and rows behind the last sequence, are not written.
+ * offsets, ret_len, src_idx, out_role and out_seg over any of k_start, k_len,
+ * reserve, role and seg_id are refused.
  */
 SONIC_API sonic_status_t sonic_kv4_compact(const uint16_t *K, const uint16_t *V,
                                            const int32_t *seg_id, const uint8_t *role,

@@ -275,6 +275,23 @@ sonic_compact_args scan_args(const sonic_kv4_cache *c, const sonic_kv4_compact_a
     return s;
 }
 
+// Whether an output lies over an input: the scan's blocks write some while others still read.
+bool outputs_over_inputs(const int32_t *seg_id, const uint8_t *role, const int32_t *offsets, const sonic_kv4_cache *c,
+                         const sonic_kv4_compact_args *a) {
+    const size_t word = sizeof(int32_t), per_seq = (size_t)a->batch * word;
+    const size_t total = (size_t)a->total_rows, rows = (size_t)c->rows;
+    const struct {
+        const void *at;
+        size_t bytes;
+    } in[] = {{a->k_start, per_seq}, {a->k_len, per_seq}, {a->reserve, per_seq}, {role, total}, {seg_id, total * word}},
+      out[] = {{offsets, per_seq + word}, {a->ret_len, per_seq}, {a->src_idx, rows * word}, {a->out_role, rows},
+               {a->out_seg, rows * word}};
+    for (const auto &o : out)
+        for (const auto &i : in)
+            if (overlap(o.at, o.bytes, i.at, i.bytes)) return true;
+    return false;
+}
+
 }  // namespace
 
 extern "C" size_t sonic_kv4_compact_workspace_size(const sonic_kv4_cache *c,
@@ -306,6 +323,7 @@ extern "C" sonic_status_t sonic_kv4_compact(const uint16_t *K, const uint16_t *V
     const sonic_compact_args s = scan_args(c, a);
     st = check_scan_workspace(&s);
     if (st != SONIC_OK) return st;
+    if (outputs_over_inputs(seg_id, role, offsets, c, a)) return SONIC_ERR_INVALID_ARGUMENT;
     int32_t *src_idx = nullptr;
     if (launch_keep_scan(seg_id, role, offsets, &s, &src_idx, stream) != cudaSuccess)
         return SONIC_ERR_CUDA;

@@ -505,7 +505,7 @@ def sonic_kv4_compact(K: torch.Tensor, V: torch.Tensor, seg_id: Optional[torch.T
                       k_len: torch.Tensor, reserve=None, ret_len=None, src_idx=None, out_role=None,
                       out_seg=None, status=None, workspace=None, stream=None):
     """sonic_compact_kv into a four-bit cache.  K, V: [n_layers, T, Hkv, D] bf16; K4, V4 as in
-    sonic_kv4_store.  Returns the workspace."""
+    sonic_kv4_store.  No output may lie over an input (ret_len is not k_len).  Returns the workspace."""
     where, dev = "sonic_kv4_compact", _device()
     lib = load()
     c, nl, hkv, rows, d = _cache(where, K4, V4, dev)

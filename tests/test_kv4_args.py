@@ -227,3 +227,23 @@ def test_evict_refuses_outputs_over_inputs():
             for at in (place[i], place[i] + (n_in - 4 if o != "out_role" else n_in - 1), place[i] - n_out + 4):
                 assert call(**{o: at}) == 1, (i, o)
     assert call(src=1 << 23) == 1
+
+
+def test_compact_refuses_outputs_over_inputs():
+    lib = sonic.load()
+    # 5 sequences, 40 rows in and 8 in the cache
+    ins = dict(k_start=20, k_len=20, reserve=20, role=40, seg=160)
+    outs = dict(offsets=24, ret_len=20, src_idx=32, out_role=8, out_seg=32)
+    place = {n: 4096 * (i + 1) for i, n in enumerate((*ins, *outs))}
+
+    def call(**at):
+        at = {**place, **at}
+        a = sonic.sonic_kv4_compact_args(5, 2, 2, 128, at["k_start"], at["k_len"], at["reserve"], 40, 10240,
+                                         at["ret_len"], at["src_idx"], at["out_role"], at["out_seg"])
+        a.workspace, a.workspace_bytes = 1 << 20, 1 << 20
+        return lib.sonic_kv4_compact(1 << 22, 1 << 23, at["seg"], at["role"], by(cache()), at["offsets"], by(a), None)
+
+    for i, n_in in ins.items():
+        for o, n_out in outs.items():
+            for at in (place[i], place[i] + (n_in - 4 if o != "out_role" else n_in - 1), place[i] - n_out + 4):
+                assert call(**{o: at}) == 1, (i, o)
