@@ -669,8 +669,9 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 mine[at] = st > 0 ? mine[at] + sum : sum;
             }
         }
-        named_barrier(1, kEpilogue);
-        if (ok && stages > 0) {
+        // a warp that gave up leaves its part of every sum out: then the block writes none of its entries
+        const bool none = named_barrier_or(1, kEpilogue, !ok);
+        if (!none && stages > 0) {
             const int64_t out = ((int64_t)u.layer * p.unit_heads + u.kvh) * p.rows + row0;
             const bool reads = p.prev != nullptr && p.keep != 0.f;
             for (int at = tid; at < u.take; at += kEpilogue) {

@@ -23,6 +23,11 @@
 #ifndef SONIC_WAIT_CHECK_MASK
 #define SONIC_WAIT_CHECK_MASK 255u
 #endif
+// Threads whose waits give up at once, as if their limit had run out (none: tests build copies of kernels with
+// some, to see the others wind down).
+#ifndef SONIC_WAIT_GIVES_UP
+#define SONIC_WAIT_GIVES_UP false
+#endif
 
 namespace sonic {
 
@@ -137,6 +142,11 @@ static __device__ __noinline__ bool mbar_wait_slow(uint64_t *bar, uint32_t parit
 // translation unit, which keeps the kernels' hot loops short.
 __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, int32_t *status,
                                           volatile int *abort) {
+    if (SONIC_WAIT_GIVES_UP) {
+        set_status(status, SONIC_ERR_DEVICE_TIMEOUT);
+        *abort = 1;
+        return false;
+    }
     if (mbar_try_wait(bar, parity)) return true;
     return mbar_wait_slow(bar, parity, status, abort);
 }
