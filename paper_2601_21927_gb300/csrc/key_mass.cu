@@ -311,13 +311,16 @@ __global__ void __launch_bounds__(kThreads, k4 && NT == 1 && !kSum ? 3 : 2) mass
     uint32_t qf[NT][D / 16][2];
     float f[NT][2], nl[NT][2];
     int limit[NT][2];  // the last key that the lane's query rows see
+    bool blind = false;  // some row saw nothing, or there is no row: the keys may hold anything for it
     auto load_q = [&](int layer, int kvh) {
+        bool sees_none = rows == 0;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = nt * 8 + g;
             const int64_t at = row < rows ? q_index(p, s, kvh, row) : 0;
             const float neg = row < rows ? neg_lse(p.lse[(int64_t)layer * p.q_rows * p.Hq + at]) : -INFINITY;
             const bool none = neg == -INFINITY;  // (a row that saw nothing may hold anything)
+            sees_none |= none && row < rows;
             uint32_t x[D / 8];
             const float back = q_words<D, k4>(p, row < rows ? p.q + layer * p.q_ls + at * D : nullptr, none, c, x);
 #pragma unroll
@@ -333,6 +336,7 @@ __global__ void __launch_bounds__(kThreads, k4 && NT == 1 && !kSum ? 3 : 2) mass
                 limit[nt][e] = __shfl_sync(0xffffffffu, sees, 8 * c + 4 * e);
             }
         }
+        blind = __any_sync(0xffffffffu, sees_none);
     };
     if (!kSum) load_q(u.layer, u.kvh);
     // lanes 4 g and 4 g + 1 write rows g and g + 8
@@ -352,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, k4 && NT == 1 && !kSum ? 3 : 2) mass
         Operand<D> o;
         make_operand<D, k4>(cur, o);
         const int pos = s.len - left - (s.len - u.from - u.take);  // the tile's first key in the sequence
-        const bool cut = pos + 16 > s.len - s.nq + 1;  // some query does not see some key
+        const bool cut = blind || pos + 16 > s.len - s.nq + 1;  // some query does not see some key
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float x[4];
@@ -541,12 +545,15 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_dead;
     __shared__ uint32_t s_top[2];
+    __shared__ int s_blind[2];  // some row of this stage saw nothing
     volatile int *abort_flag = &s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_wait();
     pdl_trigger();
     const Unit u = unit_of(p);
     if (u.take <= 0) return;
+    const Seq &s = u.s;
+    const int rows = s.nq * p.G;
     if (tid == 0) {
         for (int i = 0; i < W::kKStages; ++i) {
             mbar_init(&k_full[i], kProducer);
@@ -560,6 +567,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
         mbar_init(idle, 1);
         s_abort = 0;
         s_top[0] = s_top[1] = 0;
+        s_blind[0] = s_blind[1] = rows == 0;
         s_dead = timed_out(p.status);
         fence_mbar_init();
     }
@@ -571,8 +579,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-    const Seq &s = u.s;
-    const int rows = s.nq * p.G, row0 = s.start + u.from, last = row0 + u.take - 1;
+    const int row0 = s.start + u.from, last = row0 + u.take - 1;
     const int tiles = (u.take + kTile - 1) / kTile;
     const int chunks = max(1, (rows + N - 1) / N);
     // stage k: the query rows of one chunk of one (layer, head), against every tile
@@ -602,6 +609,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 const int64_t at = j < n ? q_index(p, s, kvh, r0 + j) : 0;
                 const float neg = j < n ? neg_lse(p.lse[(int64_t)layer * p.q_rows * p.Hq + at]) : -INFINITY;
                 const bool none = neg == -INFINITY;  // (a row that saw nothing may hold anything)
+                if (none && j < n) s_blind[st & 1] = 1;
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) {
                     uint4 w = make_uint4(0, 0, 0, 0);
@@ -649,10 +657,12 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                         sts16(q_base + swizzled(N, i >> 2, 4 * k + (i & 3)),
                               make_uint4(x[v][4 * k], x[v][4 * k + 1], x[v][4 * k + 2], x[v][4 * k + 3]));
             }
+            if (tid == 0) s_blind[st + 1 & 1] = rows == 0;  // (its readers are past the barrier above)
             fence_proxy_async_smem();
             mbar_arrive(q_full);
             // (a warp goes on, or gives up, as one: tensor memory is read by whole warps)
             ok = ok && __all_sync(0xffffffffu, mbar_wait(q_full, st & 1, p.status, abort_flag));
+            const bool blind = s_blind[st & 1];
             for (int t = 0; ok && t < tiles; ++t, ++T) {
                 const int at = t * kTile + key, pos = u.from + at;  // the key's row in the sequence
                 ok = __all_sync(0xffffffffu, mbar_wait(&s_full[T & 1], (T >> 1) & 1, p.status, abort_flag));
@@ -661,7 +671,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 // (whether some query does not see some key of the tile: a loop of its own, so that the
                 // common one has no branch between its columns)
                 const uint32_t tS = tmem + (T & 1) * (tmem_cols / 2) + ((uint32_t)(warp & 3) << 21);
-                const bool cut = u.from + t * kTile + kTile > s.len - s.nq + 1;
+                const bool cut = blind || u.from + t * kTile + kTile > s.len - s.nq + 1;
                 const float sum = cut ? sum_rows<true>(tS, 32 * part, N, f, s_nl, s_last, pos)
                                       : sum_rows<false>(tS, 32 * part, N, f, s_nl, s_last, pos);
                 tc_fence_before();

@@ -1,0 +1,52 @@
+"""Key mass where query rows are unlike: rows that saw nothing over keys that hold anything.  Against 64
+bits."""
+import pytest
+import torch
+
+from paper_2601_21927_gb300 import sonic
+from tests.test_gpu_key_mass import check_mass, make
+from tests.test_gpu_kv4 import dev, i32, status
+
+pytestmark = pytest.mark.gpu
+F = torch.float64
+
+
+def spoil(K, bits, rows):
+    """NaN in rows of the keys (in four bits: scale bytes that are NaN)."""
+    if bits == 4:
+        K[1][:, :, rows] = 255
+    else:
+        K[:, rows] = float("nan")
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+@pytest.mark.parametrize("hq,hkv,d,queries,per_head", [(8, 2, 128, 1, True), (8, 2, 64, 3, True), (24, 2, 128, 1, False),
+                                                       (28, 4, 128, 20, True), (16, 2, 64, 70, False)])
+def test_rows_that_saw_nothing_over_any_keys(bits, hq, hkv, d, queries, per_head):
+    """Sequences without a query, and with queries whose lse is -inf, keep keep * prev whatever their keys
+    hold; beside them one whose first query alone saw nothing."""
+    lens = [300, 260, 140, 150]
+    K, K64, q, lse, start, rows, nq, q_start = make(hq, hkv, d, lens, queries, bits, 2, 5)
+    nq[0] = 0
+    gone = slice(q_start[1], q_start[1] + nq[1])
+    q[:, gone], lse[:, gone] = float("nan"), -torch.inf
+    for b in (0, 1):
+        spoil(K, bits, slice(start[b], start[b] + lens[b]))
+    if nq[3] > 1:
+        q[:, q_start[3]], lse[:, q_start[3]] = float("inf"), -torch.inf
+    before = torch.rand((2, hkv if per_head else 1, rows), device=dev())
+    mass, prev, st = before.clone(), torch.rand_like(before), status()
+    sonic.sonic_key_mass(q, K, lse, i32(lens), mass, kv_start=i32(start), max_len=300, q_start=i32(q_start),
+                         q_len=i32(nq), max_q_len=queries, prev=prev, keep=0.5, status=st)
+    assert st.item() == 0
+    for b in (0, 1):
+        sl = slice(start[b], start[b] + lens[b])
+        assert torch.equal(mass[..., sl], 0.5 * prev[..., sl])
+    K64, clean = K64.clone(), q.clone()
+    for b in (0, 1):
+        K64[:, start[b]:start[b] + lens[b]] = 0
+    clean[:, gone] = 0
+    if nq[3] > 1:
+        clean[:, q_start[3]] = 0
+    nq[0], lse[:, q_start[0]] = 1, -torch.inf  # (for the check: a row that saw nothing in the place of none)
+    check_mass(mass, before, prev, 0.5, K64, clean, lse, start, lens, nq, q_start)
