@@ -602,7 +602,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
             const int layer = layer_of(st), kvh = head_of(st), r0 = st % chunks * N, n = min(N, rows - r0);
             constexpr int kItems = kWindowRows * 4 / kEpilogue;
             uint32_t x[kItems][D / 8];
-            uint32_t top = 0;  // the largest magnitude of these rows, as bf16 bits
+            uint32_t top = 0;  // the largest finite magnitude of these rows, as bf16 bits
 #pragma unroll
             for (int v = 0; v < kItems; ++v) {
                 const int i = tid + v * kEpilogue, j = i >> 2, quarter = i & 3;
@@ -628,6 +628,17 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 }
 #pragma unroll
                 for (int k = 0; k < D / 8; ++k) top = max(top, max(x[v][k] & 0x7FFFu, (x[v][k] >> 16) & 0x7FFFu));
+            }
+            if (k4 && top >= 0x7F80u) {
+                // NaN or infinities stay in their row: the others are scaled as if they were not there
+                top = 0;
+#pragma unroll
+                for (int v = 0; v < kItems; ++v)
+#pragma unroll
+                    for (int k = 0; k < D / 8; ++k) {
+                        const uint32_t lo = x[v][k] & 0x7FFFu, hi = (x[v][k] >> 16) & 0x7FFFu;
+                        top = max(top, max(lo < 0x7F80u ? lo : 0, hi < 0x7F80u ? hi : 0));
+                    }
             }
             float f = p.scale;
             if constexpr (k4) {

@@ -1,5 +1,5 @@
-"""Key mass where query rows are unlike: rows that saw nothing over keys that hold anything.  Against 64
-bits."""
+"""Key mass where query rows are unlike: rows that saw nothing over keys that hold anything, rows with
+NaN or infinities.  Against 64 bits."""
 import pytest
 import torch
 
@@ -50,3 +50,29 @@ def test_rows_that_saw_nothing_over_any_keys(bits, hq, hkv, d, queries, per_head
         clean[:, q_start[3]] = 0
     nq[0], lse[:, q_start[0]] = 1, -torch.inf  # (for the check: a row that saw nothing in the place of none)
     check_mass(mass, before, prev, 0.5, K64, clean, lse, start, lens, nq, q_start)
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+@pytest.mark.parametrize("hq,hkv,d,queries", [(8, 2, 128, 3), (28, 4, 128, 30), (16, 2, 64, 60)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_bad_row_spoils_what_it_sees(bits, hq, hkv, d, queries, value):
+    """One query row of one head holds NaN or an infinity (its lse as it comes): keys after it, and the
+    other KV heads, have their exact sums."""
+    lens = [400, 90]
+    K, K64, q, lse, start, rows, nq, q_start = make(hq, hkv, d, lens, queries, bits, 1, 9)
+    row, head = q_start[0] + 1, hq // hkv + 1  # a head of KV head 1
+    sees = lens[0] - nq[0] + 2
+    bad = q.clone()
+    bad[:, row, head, 5] = value
+    before = torch.rand((1, hkv, rows), device=dev())
+    mass = before.clone()
+    sonic.sonic_key_mass(bad, K, lse, i32(lens), mass, kv_start=i32(start), max_len=400, q_start=i32(q_start),
+                         q_len=i32(nq), max_q_len=queries, keep=0.0)
+    if value != value:
+        assert bool(mass[0, 1, start[0]:start[0] + sees].isnan().all())
+    # (what the row sees is filled in from a call without it)
+    good = before.clone()
+    sonic.sonic_key_mass(q, K, lse, i32(lens), good, kv_start=i32(start), max_len=400, q_start=i32(q_start),
+                         q_len=i32(nq), max_q_len=queries, keep=0.0)
+    mass[0, 1, start[0]:start[0] + sees] = good[0, 1, start[0]:start[0] + sees]
+    check_mass(mass, before, None, 0.0, K64, q, lse, start, lens, nq, q_start)
