@@ -37,6 +37,7 @@ constexpr int kStepRows = 16;     // query rows (queries x heads of a group) kep
 constexpr int kWindowRows = 256;  // query rows of one product
 constexpr int kRunMost = 2048;    // keys of a block
 constexpr int kTile = 128;        // keys of a step of a block: 8 warps' 16, or one product's
+constexpr uint32_t kInf16 = 0x7F80;  // bits of bf16's infinity
 
 struct Params {
     const uint16_t *q, *K;
@@ -400,10 +401,10 @@ struct Win {
     static constexpr int kOffQ = kKStages * kKBytes;  // q: [D / 64][N rows][128 bytes], swizzled
 };
 
-// Shared memory of a window kernel of N rows: operands, sums by (quarter of the rows, key), -lse and the
-// last visible key by row, barriers.
+// Shared memory of a window kernel of N rows: operands, sums by (quarter of the rows, key), -lse, the
+// last visible key and the factor to scores by row, barriers.
 struct WinLayout {
-    int acc, nl, last, bars, total;
+    int acc, nl, last, f, bars, total;
 };
 template <int D, bool k4>
 __host__ __device__ constexpr WinLayout win_layout(int N) {
@@ -411,7 +412,8 @@ __host__ __device__ constexpr WinLayout win_layout(int N) {
     w.acc = Win<D, k4>::kOffQ + N * D * 2;
     w.nl = w.acc + 4 * kRunMost * 4;
     w.last = w.nl + kWindowRows * 4;
-    w.bars = w.last + kWindowRows * 4;
+    w.f = w.last + kWindowRows * 4;
+    w.bars = w.f + kWindowRows * 4;
     w.total = w.bars + 16 * 8;
     return w;
 }
@@ -480,13 +482,13 @@ __device__ __forceinline__ void copy_tile(const Params &p, int layer, int kvh, i
 }
 
 // Sum of the weights of one key (a TMEM lane) over the 32 query rows from c0 on, and every 128th 32 after
-// them, f the factor from products to scores; kCut: rows that do not see the key add nothing.  Per
-// two rows: three packed instructions, two exponentials and half a 16-byte read of -lse.  (With a
-// factor of its own for each row the reads, 512 bytes to a warp each, were the bound: 9 clocks of
-// a scheduler per row and warp.)
-template <bool kCut>
+// them, f the factor from products to scores; kCut: rows that do not see the key add nothing; kOwn:
+// each row has a factor of its own.  Per two rows: three packed instructions, two exponentials and half a
+// 16-byte read of -lse.  (With kOwn for all tiles the reads, 512 bytes to a warp each, were the bound: 9
+// clocks of a scheduler per row and warp.)
+template <bool kCut, bool kOwn>
 __device__ __forceinline__ float sum_rows(uint32_t scores, int c0, int N, float f, const float *s_nl, const int *s_last,
-                                          int pos) {
+                                          const float *s_f, int pos) {
     const uint64_t ff = (uint64_t)__float_as_uint(f) << 32 | __float_as_uint(f);
     constexpr uint64_t kLog2e2 = 0x3FB8AA3B3FB8AA3Bull;  // log2 e twice
     uint64_t sum[2] = {0, 0};
@@ -499,6 +501,8 @@ __device__ __forceinline__ float sum_rows(uint32_t scores, int c0, int N, float 
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
             const ulonglong2 nl = *reinterpret_cast<const ulonglong2 *>(s_nl + c0 + i);
+            ulonglong2 fs = make_ulonglong2(ff, ff);
+            if (kOwn) fs = *reinterpret_cast<const ulonglong2 *>(s_f + c0 + i);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint64_t w;
@@ -507,8 +511,8 @@ __device__ __forceinline__ float sum_rows(uint32_t scores, int c0, int N, float 
                     "fma.rn.f32x2 y, x, %3, %4;\n\t"
                     "mul.rn.f32x2 %0, y, %5;\n\t}"
                     : "=l"(w)
-                    : "r"(x[i + 2 * h]), "r"(x[i + 2 * h + 1]), "l"(ff), "l"((uint64_t)(h == 0 ? nl.x : nl.y)),
-                      "l"(kLog2e2));
+                    : "r"(x[i + 2 * h]), "r"(x[i + 2 * h + 1]), "l"((uint64_t)(h == 0 ? fs.x : fs.y)),
+                      "l"((uint64_t)(h == 0 ? nl.x : nl.y)), "l"(kLog2e2));
                 float a = ex2(__uint_as_float((uint32_t)w)), b = ex2(__uint_as_float((uint32_t)(w >> 32)));
                 if (kCut) {
                     const int2 lim = *reinterpret_cast<const int2 *>(s_last + c0 + i + 2 * h);
@@ -537,6 +541,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
     float *acc = reinterpret_cast<float *>(smem + lay.acc);  // [4][kRunMost]
     float *s_nl = reinterpret_cast<float *>(smem + lay.nl);
     int *s_last = reinterpret_cast<int *>(smem + lay.last);
+    float *s_f = reinterpret_cast<float *>(smem + lay.f);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + lay.bars);
     uint64_t *k_full = bars, *k_empty = bars + W::kKStages;  // a K tile is in place / its product is done
     uint64_t *s_full = bars + 2 * W::kKStages;               // [2] a tile's scores are in their accumulator
@@ -544,7 +549,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
     uint64_t *q_full = s_empty + 2, *idle = q_full + 1;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_dead;
-    __shared__ uint32_t s_top[2];
+    __shared__ uint32_t s_top[2], s_low[2];  // the largest row of a stage, and the smallest
     __shared__ int s_blind[2];  // some row of this stage saw nothing
     volatile int *abort_flag = &s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -567,6 +572,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
         mbar_init(idle, 1);
         s_abort = 0;
         s_top[0] = s_top[1] = 0;
+        s_low[0] = s_low[1] = kInf16;
         s_blind[0] = s_blind[1] = rows == 0;
         s_dead = timed_out(p.status);
         fence_mbar_init();
@@ -602,7 +608,6 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
             const int layer = layer_of(st), kvh = head_of(st), r0 = st % chunks * N, n = min(N, rows - r0);
             constexpr int kItems = kWindowRows * 4 / kEpilogue;
             uint32_t x[kItems][D / 8];
-            uint32_t top = 0;  // the largest finite magnitude of these rows, as bf16 bits
 #pragma unroll
             for (int v = 0; v < kItems; ++v) {
                 const int i = tid + v * kEpilogue, j = i >> 2, quarter = i & 3;
@@ -626,38 +631,58 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                     s_nl[j] = neg;
                     s_last[j] = none ? -1 : s.len - s.nq + (r0 + j) / p.G;
                 }
-#pragma unroll
-                for (int k = 0; k < D / 8; ++k) top = max(top, max(x[v][k] & 0x7FFFu, (x[v][k] >> 16) & 0x7FFFu));
-            }
-            if (k4 && top >= 0x7F80u) {
-                // NaN or infinities stay in their row: the others are scaled as if they were not there
-                top = 0;
-#pragma unroll
-                for (int v = 0; v < kItems; ++v)
-#pragma unroll
-                    for (int k = 0; k < D / 8; ++k) {
-                        const uint32_t lo = x[v][k] & 0x7FFFu, hi = (x[v][k] >> 16) & 0x7FFFu;
-                        top = max(top, max(lo < 0x7F80u ? lo : 0, hi < 0x7F80u ? hi : 0));
-                    }
             }
             float f = p.scale;
+            bool alike = true;
             if constexpr (k4) {
-                // fp16, all rows scaled by 2^up so that the largest element lies in [2^13, 2^14): an element is
-                // off by at most 2^-38 of that one, so a score by no more than 2^-25 of the largest one's
-                // sum |q_d k_d| (one factor for all rows: see sum_rows)
+                // fp16, scaled by 2^up so that the largest element lies in [2^13, 2^14): one factor for all rows
+                // (see sum_rows) unless a row's largest lies more than 12 powers of two below that of another, then
+                // one for each.  So a row's largest lies at 2 or above and its elements, off by at most
+                // 2^-25, by 2^-26 of it; a score by 2^-26 max |q_d| sum |k_d| scale.
+                uint32_t own[kItems], top = 0, low = kInf16;  // largest finite magnitudes, as bf16 bits
+#pragma unroll
+                for (int v = 0; v < kItems; ++v) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int k = 0; k < D / 8; ++k) m = max(m, max(x[v][k] & 0x7FFFu, (x[v][k] >> 16) & 0x7FFFu));
+                    if (m >= kInf16) {
+                        // NaN or infinities stay in their row: all are scaled as if they were not there
+                        m = 0;
+#pragma unroll
+                        for (int k = 0; k < D / 8; ++k) {
+                            const uint32_t lo = x[v][k] & 0x7FFFu, hi = (x[v][k] >> 16) & 0x7FFFu;
+                            m = max(m, max(lo < kInf16 ? lo : 0, hi < kInf16 ? hi : 0));
+                        }
+                    }
+                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                    own[v] = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                    top = max(top, own[v]);
+                    if (own[v] > 0) low = min(low, own[v]);
+                }
                 top = __reduce_max_sync(0xffffffffu, top);
-                if (lane == 0) atomicMax(&s_top[st & 1], top);
+                low = __reduce_min_sync(0xffffffffu, low);
+                if (lane == 0) {
+                    atomicMax(&s_top[st & 1], top);
+                    atomicMin(&s_low[st & 1], low);
+                }
                 named_barrier(1, kEpilogue);
                 top = s_top[st & 1];
-                if (tid == 0) s_top[st + 1 & 1] = 0;  // (read by all before this barrier)
-                const int up = min(max(13 - ((int)(top >> 7) - 127), -126), 126);
-                const float scale = __int_as_float((127 + up) << 23);
-                f *= __int_as_float((127 - up) << 23);
+                alike = (int)(top >> 7) - (int)(s_low[st & 1] >> 7) <= 12;
+                if (tid == 0) {  // (read by all before this barrier)
+                    s_top[st + 1 & 1] = 0;
+                    s_low[st + 1 & 1] = kInf16;
+                }
 #pragma unroll
-                for (int v = 0; v < kItems; ++v)
+                for (int v = 0; v < kItems; ++v) {
+                    const int i = tid + v * kEpilogue;
+                    const int up = min(max(13 - ((int)((alike ? top : own[v]) >> 7) - 127), -126), 126);
+                    const float scale = __int_as_float((127 + up) << 23);
+                    f = p.scale * __int_as_float((127 - up) << 23);
+                    if ((i & 3) == 0 && i < N * 4) s_f[i >> 2] = f;
 #pragma unroll
                     for (int k = 0; k < D / 8; ++k)
                         x[v][k] = pack_f16x2(bf16lo(x[v][k]) * scale, bf16hi(x[v][k]) * scale);
+                }
             }
 #pragma unroll
             for (int v = 0; v < kItems; ++v) {
@@ -682,9 +707,9 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 // (whether some query does not see some key of the tile: a loop of its own, so that the
                 // common one has no branch between its columns)
                 const uint32_t tS = tmem + (T & 1) * (tmem_cols / 2) + ((uint32_t)(warp & 3) << 21);
-                const bool cut = blind || u.from + t * kTile + kTile > s.len - s.nq + 1;
-                const float sum = cut ? sum_rows<true>(tS, 32 * part, N, f, s_nl, s_last, pos)
-                                      : sum_rows<false>(tS, 32 * part, N, f, s_nl, s_last, pos);
+                const bool cut = blind || !alike || u.from + t * kTile + kTile > s.len - s.nq + 1;
+                const float sum = cut ? sum_rows<true, k4>(tS, 32 * part, N, f, s_nl, s_last, s_f, pos)
+                                      : sum_rows<false, false>(tS, 32 * part, N, f, s_nl, s_last, s_f, pos);
                 tc_fence_before();
                 mbar_arrive(&s_empty[T & 1]);
                 mine[at] = st > 0 ? mine[at] + sum : sum;
