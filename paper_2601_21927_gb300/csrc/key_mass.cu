@@ -321,7 +321,6 @@ __global__ void __launch_bounds__(kThreads, k4 && NT == 1 && !kSum ? 3 : 2) mass
             const int64_t at = row < rows ? q_index(p, s, kvh, row) : 0;
             const float neg = row < rows ? neg_lse(p.lse[(int64_t)layer * p.q_rows * p.Hq + at]) : -INFINITY;
             const bool none = neg == -INFINITY;  // (a row that saw nothing may hold anything)
-            sees_none |= none && row < rows;
             uint32_t x[D / 8];
             const float back = q_words<D, k4>(p, row < rows ? p.q + layer * p.q_ls + at * D : nullptr, none, c, x);
 #pragma unroll
@@ -335,6 +334,7 @@ __global__ void __launch_bounds__(kThreads, k4 && NT == 1 && !kSum ? 3 : 2) mass
                 f[nt][e] = __shfl_sync(0xffffffffu, back, 8 * c + 4 * e);
                 nl[nt][e] = __shfl_sync(0xffffffffu, neg, 8 * c + 4 * e);
                 limit[nt][e] = __shfl_sync(0xffffffffu, sees, 8 * c + 4 * e);
+                sees_none |= limit[nt][e] < 0 && nt * 8 + 2 * c + e < rows;
             }
         }
         blind = __any_sync(0xffffffffu, sees_none);
@@ -549,8 +549,8 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
     uint64_t *q_full = s_empty + 2, *idle = q_full + 1;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_dead;
-    __shared__ uint32_t s_top[2], s_low[2];  // the largest row of a stage, and the smallest
-    __shared__ int s_blind[2];  // some row of this stage saw nothing
+    __shared__ uint32_t s_top[2];
+    __shared__ int s_apart[2];  // some row of a stage saw nothing, or has a factor of its own
     volatile int *abort_flag = &s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_wait();
@@ -572,8 +572,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
         mbar_init(idle, 1);
         s_abort = 0;
         s_top[0] = s_top[1] = 0;
-        s_low[0] = s_low[1] = kInf16;
-        s_blind[0] = s_blind[1] = rows == 0;
+        s_apart[0] = s_apart[1] = rows == 0;
         s_dead = timed_out(p.status);
         fence_mbar_init();
     }
@@ -614,7 +613,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 const int64_t at = j < n ? q_index(p, s, kvh, r0 + j) : 0;
                 const float neg = j < n ? neg_lse(p.lse[(int64_t)layer * p.q_rows * p.Hq + at]) : -INFINITY;
                 const bool none = neg == -INFINITY;  // (a row that saw nothing may hold anything)
-                if (none && j < n) s_blind[st & 1] = 1;
+                if (none && j < n) s_apart[st & 1] = 1;
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) {
                     uint4 w = make_uint4(0, 0, 0, 0);
@@ -633,13 +632,12 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 }
             }
             float f = p.scale;
-            bool alike = true;
             if constexpr (k4) {
-                // fp16, scaled by 2^up so that the largest element lies in [2^13, 2^14): one factor for all rows
-                // (see sum_rows) unless a row's largest lies more than 12 powers of two below that of another, then
-                // one for each.  So a row's largest lies at 2 or above and its elements, off by at most
-                // 2^-25, by 2^-26 of it; a score by 2^-26 max |q_d| sum |k_d| scale.
-                uint32_t own[kItems], top = 0, low = kInf16;  // largest finite magnitudes, as bf16 bits
+                // fp16, scaled by 2^up so that the largest element lies in [2^13, 2^14): one factor for all rows (see
+                // sum_rows), but one of its own for a row whose largest lies more than 12 powers of two below.  So a
+                // row's largest lies at 2 or above and its elements, off by at most 2^-25, by 2^-26 of it;
+                // a score by 2^-26 max |q_d| sum |k_d| scale.
+                uint32_t most[kItems], top = 0;  // largest finite magnitudes, as bf16 bits: of this quarter, of all rows
 #pragma unroll
                 for (int v = 0; v < kItems; ++v) {
                     uint32_t m = 0;
@@ -654,28 +652,27 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                             m = max(m, max(lo < kInf16 ? lo : 0, hi < kInf16 ? hi : 0));
                         }
                     }
-                    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                    own[v] = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                    top = max(top, own[v]);
-                    if (own[v] > 0) low = min(low, own[v]);
+                    most[v] = m;
+                    top = max(top, m);
                 }
                 top = __reduce_max_sync(0xffffffffu, top);
-                low = __reduce_min_sync(0xffffffffu, low);
-                if (lane == 0) {
-                    atomicMax(&s_top[st & 1], top);
-                    atomicMin(&s_low[st & 1], low);
-                }
+                if (lane == 0) atomicMax(&s_top[st & 1], top);
                 named_barrier(1, kEpilogue);
                 top = s_top[st & 1];
-                alike = (int)(top >> 7) - (int)(s_low[st & 1] >> 7) <= 12;
-                if (tid == 0) {  // (read by all before this barrier)
-                    s_top[st + 1 & 1] = 0;
-                    s_low[st + 1 & 1] = kInf16;
-                }
+                if (tid == 0) s_top[st + 1 & 1] = 0;  // (read by all before this barrier)
 #pragma unroll
                 for (int v = 0; v < kItems; ++v) {
                     const int i = tid + v * kEpilogue;
-                    const int up = min(max(13 - ((int)((alike ? top : own[v]) >> 7) - 127), -126), 126);
+                    uint32_t e = top >> 7;
+                    if (__any_sync(0xffffffffu, (most[v] >> 7) + 12 < e)) {
+                        uint32_t own = max(most[v], __shfl_xor_sync(0xffffffffu, most[v], 1));
+                        own = max(own, __shfl_xor_sync(0xffffffffu, own, 2));
+                        if (own > 0 && (own >> 7) + 12 < e) {
+                            e = own >> 7;
+                            s_apart[st & 1] = 1;
+                        }
+                    }
+                    const int up = min(max(13 - ((int)e - 127), -126), 126);
                     const float scale = __int_as_float((127 + up) << 23);
                     f = p.scale * __int_as_float((127 - up) << 23);
                     if ((i & 3) == 0 && i < N * 4) s_f[i >> 2] = f;
@@ -683,6 +680,8 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                     for (int k = 0; k < D / 8; ++k)
                         x[v][k] = pack_f16x2(bf16lo(x[v][k]) * scale, bf16hi(x[v][k]) * scale);
                 }
+                const int up = min(max(13 - ((int)(top >> 7) - 127), -126), 126);
+                f = p.scale * __int_as_float((127 - up) << 23);
             }
 #pragma unroll
             for (int v = 0; v < kItems; ++v) {
@@ -693,12 +692,12 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                         sts16(q_base + swizzled(N, i >> 2, 4 * k + (i & 3)),
                               make_uint4(x[v][4 * k], x[v][4 * k + 1], x[v][4 * k + 2], x[v][4 * k + 3]));
             }
-            if (tid == 0) s_blind[st + 1 & 1] = rows == 0;  // (its readers are past the barrier above)
+            if (tid == 0) s_apart[st + 1 & 1] = rows == 0;  // (its readers are past the barrier above)
             fence_proxy_async_smem();
             mbar_arrive(q_full);
             // (a warp goes on, or gives up, as one: tensor memory is read by whole warps)
             ok = ok && __all_sync(0xffffffffu, mbar_wait(q_full, st & 1, p.status, abort_flag));
-            const bool blind = s_blind[st & 1];
+            const bool apart = s_apart[st & 1];
             for (int t = 0; ok && t < tiles; ++t, ++T) {
                 const int at = t * kTile + key, pos = u.from + at;  // the key's row in the sequence
                 ok = __all_sync(0xffffffffu, mbar_wait(&s_full[T & 1], (T >> 1) & 1, p.status, abort_flag));
@@ -707,7 +706,7 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
                 // (whether some query does not see some key of the tile: a loop of its own, so that the
                 // common one has no branch between its columns)
                 const uint32_t tS = tmem + (T & 1) * (tmem_cols / 2) + ((uint32_t)(warp & 3) << 21);
-                const bool cut = blind || !alike || u.from + t * kTile + kTile > s.len - s.nq + 1;
+                const bool cut = apart || u.from + t * kTile + kTile > s.len - s.nq + 1;
                 const float sum = cut ? sum_rows<true, k4>(tS, 32 * part, N, f, s_nl, s_last, s_f, pos)
                                       : sum_rows<false, false>(tS, 32 * part, N, f, s_nl, s_last, s_f, pos);
                 tc_fence_before();
