@@ -542,7 +542,8 @@ typedef struct {
  * order: a call repeated gives the same bits.  A sequence that falls outside
  * the rows of K or q, or with q_len[b] > lens[b], is left out (its entries as
  * they were); one longer than max_len, or with more queries than max_q_len, too.  All set
- * SONIC_ERR_INVALID_ARGUMENT in *status.
+ * SONIC_ERR_INVALID_ARGUMENT in *status.  total_kv_rows above 2^31 - 257 is
+ * unsupported.
  */
 SONIC_API sonic_status_t sonic_key_mass(const uint16_t *q, const uint16_t *K,
                                         const sonic_kv4_cache *cache, const float *lse,

@@ -37,6 +37,8 @@ constexpr int kStepRows = 16;     // query rows (queries x heads of a group) kep
 constexpr int kWindowRows = 256;  // query rows of one product
 constexpr int kRunMost = 2048;    // keys of a block
 constexpr int kTile = 128;        // keys of a step of a block: 8 warps' 16, or one product's
+// (a tile's rows are counted in 32 bits, up to a tile past a sequence's last)
+constexpr int kMostRows = 0x7fffffff - 2 * kTile;
 constexpr uint32_t kInf16 = 0x7F80;  // bits of bf16's infinity
 
 struct Params {
@@ -879,7 +881,8 @@ extern "C" sonic_status_t sonic_key_mass(const uint16_t *q, const uint16_t *K,
         if (st != SONIC_OK) return st;
         if (cache->rows != a->total_kv_rows) return SONIC_ERR_INVALID_ARGUMENT;
     }
-    if ((int64_t)std::max(a->max_q_len, 1) * (a->n_heads_q / a->n_heads_kv) > 0x7fffffffLL)
+    if (a->total_kv_rows > kMostRows ||
+        (int64_t)std::max(a->max_q_len, 1) * (a->n_heads_q / a->n_heads_kv) > 0x7fffffffLL)
         return SONIC_ERR_UNSUPPORTED;
     Params p{};
     p.q = q;

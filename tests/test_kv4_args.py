@@ -247,3 +247,13 @@ def test_compact_refuses_outputs_over_inputs():
         for o, n_out in outs.items():
             for at in (place[i], place[i] + (n_in - 4 if o != "out_role" else n_in - 1), place[i] - n_out + 4):
                 assert call(**{o: at}) == 1, (i, o)
+
+
+def test_key_mass_refuses_rows_beyond_32_bits():
+    """A tile of 128 keys reaches past a sequence's last row: its rows still have to be 32-bit numbers."""
+    lib = sonic.load()
+    for rows in (2 ** 31 - 256, 2 ** 31 - 128, 2 ** 31 - 1):
+        a = sonic.sonic_key_mass_args(2, 1, 8, 1, 64, 16, 64, rows, 0, 16, 16, 40, 80, 0, 0.0, 1, 1, None, 0.0, None)
+        assert lib.sonic_key_mass(16, 16, None, 16, 16, 16, by(a), None) == 2
+        c = sonic.sonic_kv4_cache(16, 16, None, None, rows, 0, 0)
+        assert lib.sonic_key_mass(16, None, by(c), 16, 16, 16, by(a), None) == 2
