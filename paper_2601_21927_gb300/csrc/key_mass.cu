@@ -556,7 +556,6 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
     volatile int *abort_flag = &s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_wait();
-    pdl_trigger();
     const Unit u = unit_of(p);
     if (u.take <= 0) return;
     const Seq &s = u.s;
@@ -585,6 +584,9 @@ __global__ void __launch_bounds__(kWinThreads, 1) mass_window_kernel(const Param
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // only now: a kernel behind this one may hold tensor memory while it waits for this one's end, and
+    // a block here that then asked for its own would wait for that
+    pdl_trigger();
     const uint32_t tmem = s_tmem;
     const int row0 = s.start + u.from, last = row0 + u.take - 1;
     const int tiles = (u.take + kTile - 1) / kTile;

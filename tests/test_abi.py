@@ -204,3 +204,20 @@ def test_compaction_refuses_a_misaligned_workspace():
             a.workspace = f.workspace = at
             assert lib.sonic_compact_kv(16, 16, None, 16, 16, 16, 16, ctypes.byref(a), None) == 1
             assert lib.sonic_kv4_compact(16, 16, None, 16, ctypes.byref(four), 16, ctypes.byref(f), None) == 1
+
+
+def test_tensor_memory_is_taken_before_the_next_kernel_may_start():
+    """Kernels take tensor memory ahead of waiting for the one before: that one has to hold its own by the time it
+    lets them start, or each could wait for the other."""
+    csrc = os.path.join(ROOT, "paper_2601_21927_gb300", "csrc")
+    seen = 0
+    for f in sorted(os.listdir(csrc)):
+        text = open(os.path.join(csrc, f)).read()
+        for kernel in text.split("__global__")[1:]:
+            body = kernel.split("\n}\n")[0]
+            takes = [m.start() for m in re.finditer(r"tmem_alloc\w*\(", body)]
+            lets = [m.start() for m in re.finditer(r"pdl_trigger\(\);", body)]
+            if takes and lets:
+                seen += 1
+                assert max(takes) < min(lets), (f, body[:80])
+    assert seen >= 5
