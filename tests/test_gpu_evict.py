@@ -394,3 +394,32 @@ def test_a_dialogue_in_four_bits():
     sonic.sonic_attn_decode_kv4(qs, dst[:2], dst[2:], out_len, Os, kv_start=offs[:B].contiguous(), max_len=64, status=st)
     check_decode(Os, None, qs, dst[:2], dst[2:], new_start, new_lens)
     assert st.item() == 0
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_a_second_eviction(bits):
+    """A cache whose heads chose for themselves is cut again by the weights that came out: system rows, a
+    sequence's first, and the last ones lie in the same places in every head, so they stay again."""
+    nl, hkv, d, lens = 2, 3, 64, [90, 400, 7]
+    start, rows = layout(lens)
+    role = np.full(rows, sonic.ROLE_NEXUS, np.uint8)
+    for s in start:
+        role[s:s + 6] = sonic.ROLE_SYS
+    if bits == 4:
+        src = [*random4(nl, hkv, rows, d, 3), *random4(nl, hkv, rows, d, 4)]
+    else:
+        src = [inputs.randn((nl, rows, hkv, d), k, device=dev()) for k in range(2)]
+    cap = 200
+    dst = [torch.zeros((nl, hkv, cap, x.shape[3]) if bits == 4 else (nl, cap, hkv, d), dtype=x.dtype, device=dev())
+           for x in src]
+    off, n, st = i32([0] * 4), i32([0] * 3), status()
+    mass, role_t = weights(nl, hkv, rows, 9), torch.from_numpy(role).to(dev())
+    omass = torch.zeros((nl, hkv, cap), device=dev())
+    orole = torch.zeros((nl, hkv, cap), dtype=torch.uint8, device=dev())
+    sonic.sonic_evict_kv(mass, list(zip(src, dst)), i32(lens), off, kv_start=i32(start), max_len=400,
+                         budget=i32([40, 120, 30]), reserve=i32([8, 8, 8]), role=role_t, keep_roles=1 << sonic.ROLE_SYS,
+                         recent=4, out_len=n, out_mass=omass, out_role=orole, status=st)
+    assert st.item() == 0 and n.tolist() == [40, 120, 7] and off.tolist() == [0, 48, 176, 191]
+    assert bool((orole == orole[:1, :1]).all())  # one list of roles serves every head
+    check(omass, dst, off.tolist()[:3], n.tolist(), [25, 60, 2], reserve=[8, 0, 3], role=orole[0, 0].cpu().numpy(),
+          keep_roles=1 << sonic.ROLE_SYS, recent=4)
