@@ -368,8 +368,8 @@ SONIC_API size_t sonic_decode_workspace_size(const sonic_decode_args *args);
  *       bits of exponent, one of mantissa.  Value 2i is in the lower half of
  *       byte i.
  * It stands for the values c * s, which bf16 holds exactly.  NaN is stored as
- * zero, infinities as 61440 (the rest of their block as zeros), and a block
- * whose s rounds to zero as zeros.  Rows of one KV head lie one after another
+ * zero, infinities as 61440 (their block's s is 10240: values up to 2560 beside
+ * them become zeros), and a block whose s rounds to zero as zeros.  Rows of one KV head lie one after another
  * (a generation step reads a head's rows as one stream):
  *   codes  [n_layers][n_heads_kv][rows][D / 2]
  *   scales [n_layers][n_heads_kv][rows][D / 16]
@@ -484,8 +484,9 @@ typedef struct {
  * equal shares of the keys of one KV head, and a second kernel merges the pieces of
  * sequences cut between blocks through the workspace, so concurrent calls need
  * workspaces of their own.
- * q is bf16, O bf16 (4-byte aligned), arithmetic fp32 with q (scaled per head
- * by a power of two) and the probabilities in fp16 for the products.  lens[b]
+ * The choice is made from max_len: give the longest length rather than a
+ * capacity.  q is bf16, O bf16 (4-byte aligned), arithmetic fp32 with q (scaled
+ * per head by a power of two) and the probabilities in fp16 for the products.  lens[b]
  * = 0 gives zeros (and lse = -inf).  A sequence longer than max_len is clipped
  * to it, one whose rows fall outside the cache is taken as empty; both set
  * SONIC_ERR_INVALID_ARGUMENT in *status.
@@ -536,10 +537,11 @@ typedef struct {
  * those of the last rows of a turn: what sonic_attn_decode,
  * sonic_attn_decode_kv4 or a prefill of current-turn rows over a retained
  * cache took and returned.  A row with lse = -inf (nothing visible) adds
- * nothing.  Keys are K (bf16, [n_layers][total_kv_rows][Hkv][D]) or, with K
+ * nothing, whatever it and the keys hold.  Keys are K (bf16, [n_layers][total_kv_rows][Hkv][D]) or, with K
  * NULL, the k_codes and k_scales of `cache`.  Entries outside the sequences
- * are not written; sequences must not share rows.  Sums are fp32 in a fixed
- * order: a call repeated gives the same bits.  A sequence that falls outside
+ * are not written; sequences must not share rows.  With four-bit keys the
+ * products take q in fp16, scaled by powers of two: an element is off by at most
+ * 2^-26 of its row's largest.  Sums are fp32 in a fixed order: a call repeated gives the same bits.  A sequence that falls outside
  * the rows of K or q, or with q_len[b] > lens[b], is left out (its entries as
  * they were); one longer than max_len, or with more queries than max_q_len, too.  All set
  * SONIC_ERR_INVALID_ARGUMENT in *status.  total_kv_rows above 2^31 - 257 is

@@ -15,8 +15,8 @@
 //     conversion;
 //   - one cvt and one f16x2 multiply per pair of values; the products are exact in fp16;
 //   - scores are compared with a running reference, which is only raised (a shuffle reduction and
-//     a rescale) when one exceeds it by 2^8;  P is at most 2^15 and so keeps fp16's full width
-//     down to 2^-29 of the reference.
+//     a rescale) when one exceeds it by 2^8;  P is 2^7 at the reference and at most 2^15, and so keeps
+//     fp16's full width down to 2^-21 of the reference's weight, and below that is off by 2^-32 of it.
 // tcgen05 is no help here: its operands come from shared memory, so the converted values would
 // have to be written there and fenced first (its own 4-bit types take no bf16 q and no per-row
 // scales of V).
@@ -193,7 +193,7 @@ __device__ __forceinline__ uint32_t lds_u16(uint32_t addr) {
 // State of one warp: NT groups of 8 query heads; this lane's columns are heads 2c and 2c + 1 of each.
 template <int D, int NT>
 struct State {
-    float acc[NT][D / 16][4];  // O^T: dims 16 j' ..; see write_state
+    float acc[NT][D / 16][4];  // O^T: dims 16 j' ..; see write_result
     float m[NT][2], l[NT][2];  // reference and sum (this lane's keys)
 };
 

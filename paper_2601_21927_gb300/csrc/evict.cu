@@ -32,7 +32,8 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 // Keys left that a block compares with one another instead of halving on: 64 where keys are in shared memory
 // (evict of 28 layers by head 315 us; 322 without, 370 with 256: more shared memory, a block less on each
-// SM), more where each step reads a long sequence again (60,000 rows: 427 us with 256, 441 with 64, 527 without; 347 with its loads eight at a time).
+// SM), more where each step reads a long sequence again (sequences of 60,000 and 13,978 bf16 rows, 4 layers of 4 heads
+// x 128, each choosing, 40 % kept: 427 us with 256, 441 with 64, 527 without; 347 with its loads eight at a time).
 constexpr int kFewHeld = 64, kFewLong = kThreads;
 // calls in which every select block counts for itself: role bytes read by all of them
 constexpr int64_t kSelfCount = 1 << 25;

@@ -20,8 +20,8 @@
 // the way) and sixteen take the exponentials: with eight, two to a scheduler, the chain from tensor
 // memory to the sum was waited for (85 us for eight windows of 32 rows x 7 heads over 64k keys).
 //
-// Scores: the products of bf16 (or fp16: four-bit values and q scaled by a power of two) are exact;
-// fp32 sums.  scale s - lse is formed before the factor log2 e, so its rounding is relative to the
+// Scores: the products of bf16 are exact, and those of fp16 (four-bit values, and q scaled by a power of two
+// that its larger elements hold all their bits) but for q's rounding; fp32 sums.  scale s - lse is formed before the factor log2 e, so its rounding is relative to the
 // small difference.
 #include <algorithm>
 
@@ -48,7 +48,7 @@ struct Params {
     float *mass;
     const int32_t *lens, *kv_start, *q_start, *q_len;
     int32_t *status;
-    int32_t B, Hq, Hkv, G, n_layers, rows, q_rows, max_len, max_q_len;
+    int32_t B, Hq, Hkv, G, rows, q_rows, max_len, max_q_len;
     int32_t run, runs;                // keys of a block; blocks per (layer, sequence, KV head)
     int32_t unit_layers, sum_layers;  // layers with a block each; layers added up (one of them is 1)
     int32_t unit_heads, sum_heads;    // the same of KV heads
@@ -907,7 +907,6 @@ extern "C" sonic_status_t sonic_key_mass(const uint16_t *q, const uint16_t *K,
     p.Hq = a->n_heads_q;
     p.Hkv = a->n_heads_kv;
     p.G = a->n_heads_q / a->n_heads_kv;
-    p.n_layers = a->n_layers;
     p.rows = a->total_kv_rows;
     p.q_rows = a->total_q_rows;
     p.max_len = a->max_len;

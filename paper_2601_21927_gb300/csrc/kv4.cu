@@ -34,7 +34,7 @@ struct RowParams {
 };
 
 // 32 bytes: in one access where every row starts on 32 bytes, else in two.  (Two 16-byte stores of
-// a warp each fill half of their sectors: unpacking ran at 4.5 TB/s with L2 at 63 %.)
+// a warp each fill half of their sectors: unpacking ran at 4.7 TB/s with L2 at 63 %.)
 __device__ __forceinline__ void load32(uint32_t (&w)[8], const void *p, bool whole) {
     if (whole) {
         asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"

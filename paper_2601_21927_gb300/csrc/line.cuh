@@ -1,4 +1,4 @@
-// The line of keys that persistent blocks share out (attention over four-bit caches, key mass).
+// The line of keys that persistent blocks share out (attention over four-bit caches).
 //
 // The keys of all (layer, sequence) pairs, layer-major and the sequences' lengths one after
 // another, form one line of n = layers * sum keys; block group g takes keys

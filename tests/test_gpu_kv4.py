@@ -506,3 +506,18 @@ def test_binding_refuses():
         with pytest.raises(sonic.SonicError):
             sonic.sonic_attn_decode_kv4(a["q"], K4, V4, a["lens"], a["O"], kv_start=a["kv_start"], max_len=5,
                                         lse=a["lse"])
+
+
+def test_what_stands_beside_an_infinity():
+    """An infinity's block has the largest scale, 10240: what lies beside it keeps a code from a quarter of that on."""
+    row = [float("inf"), 20000.0, 2560.0, 2576.0, -2560.0, -2576.0, 7680.0, 7712.0, 61440.0, 3e38, -3e38, 1.0, 0.0, 12800.0,
+           17920.0, -float("inf")]
+    K = torch.tensor(row * 4, dtype=torch.bfloat16, device=dev()).view(1, 1, 1, 64)
+    K4, V4 = empty4(1, 1, 1, 64), empty4(1, 1, 1, 64)
+    oK, oV = torch.empty_like(K), torch.empty_like(K)
+    sonic.sonic_kv4_store(K, K, K4, V4)
+    sonic.sonic_kv4_load(K4, V4, oK, oV)
+    assert bool((K4[1] == 226).all())
+    want = plain.decode(*plain.encode(K.transpose(1, 2))).transpose(1, 2)
+    assert torch.equal(oK.cpu().double(), want) and torch.equal(oV.cpu().double(), want)
+    assert want.flatten()[:6].tolist() == [61440, 20480, 0, 5120, 0, -5120]
