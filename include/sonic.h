@@ -166,8 +166,9 @@ typedef struct {
  * offsets[b] + j of layer l of out_K (resp. out_V), bit for bit.  Reserve
  * rows are not written, and no output may overlap an input.  seg_id may be
  * NULL; when given it is checked (non-decreasing within a sequence, no body row
- * in segment 0) and a violation sets SONIC_ERR_LAYOUT.  If offsets[B] > out_capacity_rows the
- * call sets SONIC_ERR_CAPACITY and copies only rows below the capacity.
+ * in segment 0) and a violation sets SONIC_ERR_LAYOUT.  If offsets[B] >
+ * out_capacity_rows the call sets SONIC_ERR_CAPACITY and copies only rows below
+ * the capacity.
  * K/V/out pointers must be 16-byte aligned.  B > 65535 or n_layers > 32767
  * returns SONIC_ERR_UNSUPPORTED.  A sequence whose rows fall outside
  * [0, total_rows) keeps no rows (ret_len 0) and sets
@@ -537,15 +538,16 @@ typedef struct {
  * those of the last rows of a turn: what sonic_attn_decode,
  * sonic_attn_decode_kv4 or a prefill of current-turn rows over a retained
  * cache took and returned.  A row with lse = -inf (nothing visible) adds
- * nothing, whatever it and the keys hold.  Keys are K (bf16, [n_layers][total_kv_rows][Hkv][D]) or, with K
- * NULL, the k_codes and k_scales of `cache`.  Entries outside the sequences
- * are not written; sequences must not share rows.  With four-bit keys the
- * products take q in fp16, scaled by powers of two: an element is off by at most
- * 2^-26 of its row's largest.  Sums are fp32 in a fixed order: a call repeated gives the same bits.  A sequence that falls outside
- * the rows of K or q, or with q_len[b] > lens[b], is left out (its entries as
- * they were); one longer than max_len, or with more queries than max_q_len, too.  All set
- * SONIC_ERR_INVALID_ARGUMENT in *status.  total_kv_rows above 2^31 - 257 is
- * unsupported.
+ * nothing, whatever it and the keys hold.  Keys are K (bf16, [n_layers]
+ * [total_kv_rows][Hkv][D]) or, with K NULL, the k_codes and k_scales of `cache`.
+ * Entries outside the sequences are not written; sequences must not share rows.
+ * With four-bit keys the products take q in fp16, scaled by powers of two: an
+ * element is off by at most 2^-26 of its row's largest.  Sums are fp32 in a
+ * fixed order: a call repeated gives the same bits.  A sequence that falls
+ * outside the rows of K or q, or with q_len[b] > lens[b], is left out (its
+ * entries as they were); one longer than max_len, or with more queries than
+ * max_q_len, too.  All set SONIC_ERR_INVALID_ARGUMENT in *status.
+ * total_kv_rows above 2^31 - 257 is unsupported.
  */
 SONIC_API sonic_status_t sonic_key_mass(const uint16_t *q, const uint16_t *K,
                                         const sonic_kv4_cache *cache, const float *lse,
